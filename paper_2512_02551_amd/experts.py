@@ -216,15 +216,18 @@ def _torch_type(name: str):
 
 
 def _rows(t, what: str, dims: int = 2):
-    """(pointer, leading dimension) of a CUDA tensor whose rows are contiguous."""
+    """(tensor, leading dimension) of a CUDA tensor whose rows are contiguous.  Rows that share memory -- one repeated by expand(), say -- have no leading
+    dimension: they are copied apart.  The caller holds the tensor until its kernel is enqueued."""
     if not t.is_cuda:
         raise TypeError(f"{what}: a CUDA tensor is needed")
     if t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
         raise ValueError(f"{what}: {dims} dimensions with contiguous rows are needed")
+    if t.shape[-2] > 1 and t.stride(-2) < t.shape[-1]:
+        t = t.contiguous()
     ld = max(t.stride(-2), t.shape[-1], 1)
     if dims == 3 and t.shape[0] > 1 and t.stride(0) != t.shape[1] * ld:
         raise ValueError(f"{what}: packed groups are needed")
-    return t.data_ptr(), ld
+    return t, ld
 
 
 def _ints(t, what: str, *shape):
@@ -254,7 +257,7 @@ def quantise(x, q: str = "e4m3", scale: str = "f32", block_rows: int = 1, rows: 
     Q is [M][K rounded up to 16], its tail zeros; S is [blocks of K][M], for block_rows = 128 [blocks of M][blocks of K]."""
     import torch
 
-    px, ldx = _rows(x, "x")
+    x, ldx = _rows(x, "x")
     m, k = (x.shape[0] if index is None else index.shape[0]), x.shape[1]
     pi = 0 if index is None else _ints(index, "index", m)
     p = QuantisePlan(m, k, _type_name(x), q, scale, block_rows, x_rows=0 if index is None else x.shape[0], ldx=ldx)
@@ -266,7 +269,7 @@ def quantise(x, q: str = "e4m3", scale: str = "f32", block_rows: int = 1, rows: 
     if transposed:
         qt, st = new((k, _up16(m)), bytes_), new((_blocks(k), _blocks(m)) if block_rows > 1 else (_blocks(m), k), kind)
     at = lambda t: 0 if t is None else t.data_ptr()  # noqa: E731
-    p.run(px, at(qs), at(ss), at(qt), at(st), _stream(), pi)
+    p.run(x.data_ptr(), at(qs), at(ss), at(qt), at(st), _stream(), pi)
     return qs, ss, qt, st
 
 
@@ -288,8 +291,8 @@ def scaled_product(a, scale_a, b, scale_b, K: Optional[int] = None, c: str = "f1
     pi = 0 if index is None else _ints(index, "index", M)
     if index is not None and not by_rows:
         raise ValueError("an index needs groups of rows")
-    (pa, lda), (pb, ldb) = _rows(a, "a"), _rows(b, "b", 3 if by_rows else 2)
-    (psa, ldsa), (psb, ldsb) = _rows(scale_a, "scale_a"), _rows(scale_b, "scale_b", 3 if by_rows else 2)
+    (a, lda), (b, ldb) = _rows(a, "a"), _rows(b, "b", 3 if by_rows else 2)
+    (scale_a, ldsa), (scale_b, ldsb) = _rows(scale_a, "scale_a"), _rows(scale_b, "scale_b", 3 if by_rows else 2)
     by_block = tuple(scale_b.shape[-2:]) == (_blocks(N), _blocks(K))
     if by_rows and (b.shape[0] != groups or scale_b.shape[0] != groups):
         raise ValueError("b and scale_b hold one matrix for each group")
@@ -300,7 +303,7 @@ def scaled_product(a, scale_a, b, scale_b, K: Optional[int] = None, c: str = "f1
         raise ValueError("scale_a has another shape")
     out = torch.empty((groups, M, N) if groups and not by_rows else (M, N), dtype=_torch_type(c), device=a.device)
     with ScaledPlan(M, N, K, _type_name(a), c, _type_name(scale_a), SCALE_BLOCK if by_block else 1, groups, along, a.shape[0] if index is not None else 0, lda, ldb, 0, ldsa, ldsb, spec) as p:
-        p.run(pa, psa, pb, psb, out.data_ptr(), _stream(), po, pi)
+        p.run(a.data_ptr(), scale_a.data_ptr(), b.data_ptr(), scale_b.data_ptr(), out.data_ptr(), _stream(), po, pi)
         if p.workspace_bytes():
             torch.cuda.current_stream().synchronize()     # the plan's workspace is freed on exit
     return out
@@ -310,7 +313,7 @@ def route(logits, k: int, bias=None, score: str = "softmax", groups: int = 1, ke
     """logits [tokens][experts] -> weights [tokens][k], experts [tokens][k], offsets [experts + 1], rows [tokens][k], tokens_of [capacity]."""
     import torch
 
-    pl, ld = _rows(logits, "logits")
+    logits, ld = _rows(logits, "logits")
     t, e = logits.shape
     new = lambda dtype, *shape: torch.empty(shape, dtype=dtype, device=logits.device)  # noqa: E731
     if bias is not None and (bias.dtype != torch.float32 or not bias.is_cuda or not bias.is_contiguous() or tuple(bias.shape) != (e,)):
@@ -318,7 +321,7 @@ def route(logits, k: int, bias=None, score: str = "softmax", groups: int = 1, ke
     with RoutePlan(t, e, k, _type_name(logits), score, groups, keep, top2, renormalise, factor, align, ld) as p:
         weights, experts = new(torch.float32, t, k), new(torch.int32, t, k)
         offsets, rows, tokens_of = new(torch.int32, e + 1), new(torch.int32, t, k), new(torch.int32, p.capacity)
-        p.run(pl, 0 if bias is None else bias.data_ptr(), weights.data_ptr(), experts.data_ptr(), offsets.data_ptr(), rows.data_ptr(), tokens_of.data_ptr(), _stream())
+        p.run(logits.data_ptr(), 0 if bias is None else bias.data_ptr(), weights.data_ptr(), experts.data_ptr(), offsets.data_ptr(), rows.data_ptr(), tokens_of.data_ptr(), _stream())
         torch.cuda.current_stream().synchronize()         # the plan's workspace is freed on exit
     return weights, experts, offsets, rows, tokens_of
 
@@ -327,14 +330,14 @@ def route_backward(logits, experts, dweights, score: str = "softmax", renormalis
     """dlogits from the gradient of route()'s weights, given its choice."""
     import torch
 
-    pl, ld = _rows(logits, "logits")
+    logits, ld = _rows(logits, "logits")
     t, k = experts.shape
     pe = _ints(experts, "experts", logits.shape[0], k)
     if dweights.dtype != torch.float32 or not dweights.is_cuda or not dweights.is_contiguous() or dweights.shape != experts.shape:
         raise TypeError("dweights: a contiguous float32 CUDA tensor of the shape of experts is needed")
     dlogits = torch.empty_strided(logits.shape, (ld, 1), dtype=logits.dtype, device=logits.device)
     with RoutePlan(t, logits.shape[1], k, _type_name(logits), score, renormalise=renormalise, factor=factor, ld=ld) as p:
-        p.backward(pl, pe, dweights.data_ptr(), dlogits.data_ptr(), _stream())
+        p.backward(logits.data_ptr(), pe, dweights.data_ptr(), dlogits.data_ptr(), _stream())
         torch.cuda.current_stream().synchronize()         # the plan's workspace is freed on exit
     return dlogits
 
@@ -343,13 +346,13 @@ def combine(y, rows, weights=None, out: Optional[str] = None):
     """out[t] = sum over j of weights[t][j] * y[rows[t][j]]; weights None: ones."""
     import torch
 
-    py, ldy = _rows(y, "y")
+    y, ldy = _rows(y, "y")
     t, k = rows.shape
     pr = _ints(rows, "rows", t, k)
     if weights is not None and (weights.dtype != torch.float32 or not weights.is_contiguous() or weights.shape != rows.shape):
         raise TypeError("weights: a contiguous float32 tensor of the shape of rows is needed")
     found = torch.empty((t, y.shape[1]), dtype=y.dtype if out is None else _torch_type(out), device=y.device)
-    CombinePlan(t, k, y.shape[1], y.shape[0], _type_name(y), _type_name(found), ldy).run(pr, 0 if weights is None else weights.data_ptr(), py, found.data_ptr(), _stream())
+    CombinePlan(t, k, y.shape[1], y.shape[0], _type_name(y), _type_name(found), ldy).run(pr, 0 if weights is None else weights.data_ptr(), y.data_ptr(), found.data_ptr(), _stream())
     return found
 
 
@@ -357,16 +360,16 @@ def combine_backward(y, rows, tokens_of, weights, dout):
     """(dY, dweights) of combine(y, rows, weights)."""
     import torch
 
-    py, ldy = _rows(y, "y")
-    pd, ldo = _rows(dout, "dout")
+    y, ldy = _rows(y, "y")
+    dout, ldo = _rows(dout, "dout")
     t, k = rows.shape
     pr, pt = _ints(rows, "rows", t, k), _ints(tokens_of, "tokens_of", y.shape[0])
     if weights is not None and (weights.dtype != torch.float32 or not weights.is_contiguous() or weights.shape != rows.shape):
         raise TypeError("weights: a contiguous float32 tensor of the shape of rows is needed")
     if tuple(dout.shape) != (t, y.shape[1]):
         raise ValueError("dout has another shape")
-    dy = torch.empty_strided(y.shape, y.stride(), dtype=y.dtype, device=y.device)
+    dy = torch.empty_strided(y.shape, (ldy, 1), dtype=y.dtype, device=y.device)
     dw = torch.empty((t, k), dtype=torch.float32, device=y.device)
     CombinePlan(t, k, y.shape[1], y.shape[0], _type_name(y), _type_name(dout), ldy, ldo).backward(
-        pr, pt, 0 if weights is None else weights.data_ptr(), py, pd, dy.data_ptr(), dw.data_ptr(), _stream())
+        pr, pt, 0 if weights is None else weights.data_ptr(), y.data_ptr(), dout.data_ptr(), dy.data_ptr(), dw.data_ptr(), _stream())
     return dy, dw

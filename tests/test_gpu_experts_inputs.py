@@ -1,0 +1,62 @@
+"""The expert-layer operators on inputs off the ordinary: rows that share memory."""
+import zlib
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2512_02551_amd as hg  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+
+
+def gen(*seed):
+    g = torch.Generator()
+    g.manual_seed(zlib.crc32(repr(seed).encode()))
+    return g
+
+
+def same(got, want):
+    """Bit for bit (no NaN among them)."""
+    return all(a is b is None or torch.equal(a.float(), b.float()) for a, b in zip(got, want))
+
+
+# ---- rows that share memory: the results of the same values in rows of their own -----------------------------------------------------
+
+SHARED = {"repeated": 0, "overlapping": 40}
+
+
+def shared(name, rows, cols, dtype, g):
+    base = torch.randn(rows * 40 + cols, generator=g).to(dtype).cuda()
+    x = torch.as_strided(base, (rows, cols), (SHARED[name], 1))
+    return x, x.contiguous()
+
+
+@pytest.mark.parametrize("name", list(SHARED))
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32], ids=str)
+def test_rows_that_share_memory(name, dtype):
+    g = gen("shared", name, dtype)
+    x, own = shared(name, 70, 256, dtype, g)
+    assert same(hg.quantise(x, transposed=True), hg.quantise(own, transposed=True))
+    assert same(hg.quantise(x, block_rows=128, transposed=True), hg.quantise(own, block_rows=128, transposed=True))
+    found, want = hg.route(x, 4), hg.route(own, 4)
+    assert same(found, want)
+    dw = torch.randn((70, 4), generator=g).cuda()
+    assert torch.equal(hg.route_backward(x, found[1], dw), hg.route_backward(own, found[1], dw))
+    rows = torch.randperm(70, generator=g).to(torch.int32).view(35, 2).cuda()
+    tokens = torch.empty(70, dtype=torch.int32, device="cuda")
+    tokens[rows.flatten().long()] = torch.arange(35, dtype=torch.int32, device="cuda").repeat_interleave(2)
+    w = torch.rand((35, 2), generator=g).cuda()
+    assert torch.equal(hg.combine(x, rows, w), hg.combine(own, rows, w))
+    dout, dout_own = shared(name, 35, 256, dtype, g)
+    assert same(hg.combine_backward(x, rows, tokens, w, dout), hg.combine_backward(own, rows, tokens, w, dout_own))
+
+
+@pytest.mark.parametrize("name", list(SHARED))
+def test_operands_of_a_product_that_share_memory(name):
+    g = gen("shared operands", name)
+    a, b = (torch.as_strided((torch.randn(8192, generator=g) * 4).to(torch.float8_e4m3fn).cuda(), (r, 384), (SHARED[name] // 16 * 16, 1)) for r in (50, 60))
+    own = [t.view(torch.uint8).contiguous().view(torch.float8_e4m3fn) for t in (a, b)]
+    sa, sb = (torch.rand((1, r), generator=g).cuda().expand(3, r) for r in (50, 60))      # one scale for all blocks of a row
+    found = hg.scaled_product(a, sa, b, sb, c="f32")
+    assert torch.equal(found, hg.scaled_product(own[0], sa.contiguous(), own[1], sb.contiguous(), c="f32")) and found.abs().max() > 0
