@@ -230,12 +230,23 @@ def _rows(t, what: str, dims: int = 2):
     return t, ld
 
 
-def _ints(t, what: str, *shape):
+def _whole(t, what: str, dtype: str, shape) -> int:
+    """Address of a contiguous CUDA tensor of one type and shape; None: a null pointer."""
     import torch
 
-    if t.dtype != torch.int32 or not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != shape:
-        raise TypeError(f"{what}: a contiguous int32 CUDA tensor of shape {shape} is needed")
+    if t is None:
+        return 0
+    if t.dtype != getattr(torch, dtype) or not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != tuple(shape):
+        raise TypeError(f"{what}: a contiguous {dtype} CUDA tensor of shape {tuple(shape)} is needed")
     return t.data_ptr()
+
+
+def _ints(t, what: str, *shape) -> int:
+    return _whole(t, what, "int32", shape)
+
+
+def _floats(t, what: str, *shape) -> int:
+    return _whole(t, what, "float32", shape)
 
 
 def _stream() -> int:
@@ -316,12 +327,11 @@ def route(logits, k: int, bias=None, score: str = "softmax", groups: int = 1, ke
     logits, ld = _rows(logits, "logits")
     t, e = logits.shape
     new = lambda dtype, *shape: torch.empty(shape, dtype=dtype, device=logits.device)  # noqa: E731
-    if bias is not None and (bias.dtype != torch.float32 or not bias.is_cuda or not bias.is_contiguous() or tuple(bias.shape) != (e,)):
-        raise TypeError("bias: a contiguous float32 CUDA tensor with a value for each expert is needed")
+    pb = _floats(bias, "bias", e)
     with RoutePlan(t, e, k, _type_name(logits), score, groups, keep, top2, renormalise, factor, align, ld) as p:
         weights, experts = new(torch.float32, t, k), new(torch.int32, t, k)
         offsets, rows, tokens_of = new(torch.int32, e + 1), new(torch.int32, t, k), new(torch.int32, p.capacity)
-        p.run(logits.data_ptr(), 0 if bias is None else bias.data_ptr(), weights.data_ptr(), experts.data_ptr(), offsets.data_ptr(), rows.data_ptr(), tokens_of.data_ptr(), _stream())
+        p.run(logits.data_ptr(), pb, weights.data_ptr(), experts.data_ptr(), offsets.data_ptr(), rows.data_ptr(), tokens_of.data_ptr(), _stream())
         torch.cuda.current_stream().synchronize()         # the plan's workspace is freed on exit
     return weights, experts, offsets, rows, tokens_of
 
@@ -333,11 +343,10 @@ def route_backward(logits, experts, dweights, score: str = "softmax", renormalis
     logits, ld = _rows(logits, "logits")
     t, k = experts.shape
     pe = _ints(experts, "experts", logits.shape[0], k)
-    if dweights.dtype != torch.float32 or not dweights.is_cuda or not dweights.is_contiguous() or dweights.shape != experts.shape:
-        raise TypeError("dweights: a contiguous float32 CUDA tensor of the shape of experts is needed")
+    pw = _floats(dweights, "dweights", t, k)
     dlogits = torch.empty_strided(logits.shape, (ld, 1), dtype=logits.dtype, device=logits.device)
     with RoutePlan(t, logits.shape[1], k, _type_name(logits), score, renormalise=renormalise, factor=factor, ld=ld) as p:
-        p.backward(logits.data_ptr(), pe, dweights.data_ptr(), dlogits.data_ptr(), _stream())
+        p.backward(logits.data_ptr(), pe, pw, dlogits.data_ptr(), _stream())
         torch.cuda.current_stream().synchronize()         # the plan's workspace is freed on exit
     return dlogits
 
@@ -348,11 +357,9 @@ def combine(y, rows, weights=None, out: Optional[str] = None):
 
     y, ldy = _rows(y, "y")
     t, k = rows.shape
-    pr = _ints(rows, "rows", t, k)
-    if weights is not None and (weights.dtype != torch.float32 or not weights.is_contiguous() or weights.shape != rows.shape):
-        raise TypeError("weights: a contiguous float32 tensor of the shape of rows is needed")
+    pr, pw = _ints(rows, "rows", t, k), _floats(weights, "weights", t, k)
     found = torch.empty((t, y.shape[1]), dtype=y.dtype if out is None else _torch_type(out), device=y.device)
-    CombinePlan(t, k, y.shape[1], y.shape[0], _type_name(y), _type_name(found), ldy).run(pr, 0 if weights is None else weights.data_ptr(), y.data_ptr(), found.data_ptr(), _stream())
+    CombinePlan(t, k, y.shape[1], y.shape[0], _type_name(y), _type_name(found), ldy).run(pr, pw, y.data_ptr(), found.data_ptr(), _stream())
     return found
 
 
@@ -363,13 +370,11 @@ def combine_backward(y, rows, tokens_of, weights, dout):
     y, ldy = _rows(y, "y")
     dout, ldo = _rows(dout, "dout")
     t, k = rows.shape
-    pr, pt = _ints(rows, "rows", t, k), _ints(tokens_of, "tokens_of", y.shape[0])
-    if weights is not None and (weights.dtype != torch.float32 or not weights.is_contiguous() or weights.shape != rows.shape):
-        raise TypeError("weights: a contiguous float32 tensor of the shape of rows is needed")
+    pr, pt, pw = _ints(rows, "rows", t, k), _ints(tokens_of, "tokens_of", y.shape[0]), _floats(weights, "weights", t, k)
     if tuple(dout.shape) != (t, y.shape[1]):
         raise ValueError("dout has another shape")
     dy = torch.empty_strided(y.shape, (ldy, 1), dtype=y.dtype, device=y.device)
     dw = torch.empty((t, k), dtype=torch.float32, device=y.device)
     CombinePlan(t, k, y.shape[1], y.shape[0], _type_name(y), _type_name(dout), ldy, ldo).backward(
-        pr, pt, 0 if weights is None else weights.data_ptr(), y.data_ptr(), dout.data_ptr(), dy.data_ptr(), dw.data_ptr(), _stream())
+        pr, pt, pw, y.data_ptr(), dout.data_ptr(), dy.data_ptr(), dw.data_ptr(), _stream())
     return dy, dw

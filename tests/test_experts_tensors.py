@@ -168,3 +168,20 @@ def test_groups_have_to_be_packed(library):
         with pytest.raises(ValueError, match="packed groups"):
             hg.scaled_product(a, device(torch.ones(1, 4)), device(shared), scales, offsets=offsets)
         assert library.launches == before
+
+
+@pytest.mark.parametrize("wrong", ["on the host", "of another type", "of another shape", "not contiguous"])
+@pytest.mark.parametrize("function", ["combine", "combine_backward", "route", "route_backward"])
+def test_weights_are_checked_before_a_kernel_sees_them(library, function, wrong):
+    t, k = 4, 2
+    good = (3,) if function == "route" else (t, k)
+    bad = {"on the host": torch.ones(good), "of another type": device(torch.ones(good, dtype=torch.float16)), "of another shape": device(torch.ones(5, 7)),
+           "not contiguous": device(torch.ones(*good, 2)[..., 0])}[wrong]
+    y, logits = view("packed"), device(torch.randn(t, 3))
+    call = {"combine": lambda w: hg.combine(y, ints(t, k), w), "combine_backward": lambda w: hg.combine_backward(y, ints(t, k), ints(ROWS), w, device(torch.ones(t, COLS))),
+            "route": lambda w: hg.route(logits, k, w), "route_backward": lambda w: hg.route_backward(logits, ints(t, k), w)}[function]
+    with pytest.raises(TypeError):
+        call(bad)
+    assert library.launches == 0
+    call(device(torch.ones(good)))
+    assert library.launches == 1
