@@ -2,7 +2,7 @@
 quantising, routing and combining.  Argument marshalling only.
 
 The ``*Plan`` classes take raw device pointers and a stream, as :class:`~paper_2512_02551_amd.Plan` does; the lower-case functions take
-torch tensors, allocate the results and run on torch's current stream.
+torch tensors on the current device, allocate the results and run on torch's current stream.
 """
 from __future__ import annotations
 
@@ -215,11 +215,20 @@ def _torch_type(name: str):
     return {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32, "e4m3": torch.float8_e4m3fn, "e5m2": torch.float8_e5m2, "e8m0": torch.uint8}[name]
 
 
+def _on_device(t, what: str) -> None:
+    """The kernels go to the current device's stream: its memory is what they reach."""
+    import torch
+
+    if not t.is_cuda:
+        raise TypeError(f"{what}: a CUDA tensor is needed")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{what}: on cuda:{t.get_device()}, and the current device is cuda:{torch.cuda.current_device()}")
+
+
 def _rows(t, what: str, dims: int = 2):
     """(tensor, leading dimension) of a CUDA tensor whose rows are contiguous.  Rows that share memory -- one repeated by expand(), say -- have no leading
     dimension: they are copied apart.  The caller holds the tensor until its kernel is enqueued."""
-    if not t.is_cuda:
-        raise TypeError(f"{what}: a CUDA tensor is needed")
+    _on_device(t, what)
     if t.dim() != dims or (t.shape[-1] > 1 and t.stride(-1) != 1):
         raise ValueError(f"{what}: {dims} dimensions with contiguous rows are needed")
     if t.shape[-2] > 1 and t.stride(-2) < t.shape[-1]:
@@ -238,6 +247,7 @@ def _whole(t, what: str, dtype: str, shape) -> int:
         return 0
     if t.dtype != getattr(torch, dtype) or not t.is_cuda or not t.is_contiguous() or tuple(t.shape) != tuple(shape):
         raise TypeError(f"{what}: a contiguous {dtype} CUDA tensor of shape {tuple(shape)} is needed")
+    _on_device(t, what)
     return t.data_ptr()
 
 

@@ -14,9 +14,14 @@ DTYPES = [torch.float16, torch.bfloat16, torch.float32]          # of hgemm_type
 
 
 class Device(torch.Tensor):
-    """A host tensor that claims to be on the GPU."""
+    """A host tensor that claims to be on a GPU."""
 
     is_cuda = property(lambda self: True)
+    get_device = lambda self: 0  # noqa: E731
+
+
+class OtherDevice(Device):
+    get_device = lambda self: 1  # noqa: E731
 
 
 def device(t):
@@ -97,6 +102,7 @@ class Library:
 def library(monkeypatch):
     lib = Library()
     monkeypatch.setattr(experts, "_lib", lambda: lib)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: types.SimpleNamespace(cuda_stream=0, synchronize=lambda: None))
     return lib
 
@@ -185,3 +191,28 @@ def test_weights_are_checked_before_a_kernel_sees_them(library, function, wrong)
     assert library.launches == 0
     call(device(torch.ones(good)))
     assert library.launches == 1
+
+
+def test_tensors_of_another_device_are_refused(library, monkeypatch):
+    """Each operand in turn on device 1 with device 0 current, and all of them on device 0 with device 1 current."""
+    q = lambda *shape: device(torch.ones(shape, dtype=torch.float8_e4m3fn))  # noqa: E731
+    f = lambda *shape: device(torch.ones(shape))  # noqa: E731
+    calls = [
+        (lambda x, index: hg.quantise(x, index=index), [f(4, COLS), ints(6)]),
+        (hg.scaled_product, [q(4, COLS), f(1, 4), q(5, COLS), f(1, 1)]),
+        (lambda a, sa, b, sb, o, i: hg.scaled_product(a, sa, b, sb, offsets=o, index=i), [q(4, COLS), f(1, 4), q(2, 5, COLS), f(2, 1, 1), ints(3), ints(6)]),
+        (lambda x, b: hg.route(x, 2, b), [f(4, 8), f(8)]), (hg.route_backward, [f(4, 8), ints(4, 2), f(4, 2)]),
+        (hg.combine, [f(6, COLS), ints(4, 2), f(4, 2)]), (hg.combine_backward, [f(6, COLS), ints(4, 2), ints(6), f(4, 2), f(4, COLS)]),
+    ]
+    for n, (function, operands) in enumerate(calls):
+        function(*operands)
+        assert library.launches == n + 1
+    for function, operands in calls:
+        for i in range(len(operands)):
+            with pytest.raises(ValueError, match="cuda:1"):
+                function(*operands[:i], operands[i].as_subclass(OtherDevice), *operands[i + 1:])
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    for function, operands in calls:
+        with pytest.raises(ValueError, match="cuda:1"):
+            function(*operands)
+    assert library.launches == len(calls)
