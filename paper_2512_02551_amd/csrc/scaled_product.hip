@@ -243,8 +243,9 @@ hgemm_status_t make_plan_unguarded(hgemm_scaled_plan_t* out, int64_t M, int64_t 
         p->grid_y = a.group == HGEMM_GROUPS_DEPTH ? a.groups : 1;
         p->kernel = c.entry->kernel[sum_of(a)][desc->a][a.b_by_row];
         g.splits = 1;
-        if (c.sk > 1 && a.group == HGEMM_GROUPS_NONE) {
-            const int64_t blocks = blocks_of(K), each = (blocks + c.sk - 1) / c.sk;
+        const int64_t blocks = blocks_of(K);
+        if (c.sk > 1 && blocks > 1 && a.group == HGEMM_GROUPS_NONE) {
+            const int64_t each = (blocks + c.sk - 1) / c.sk;
             g.splits = (int)((blocks + each - 1) / each);       // no range is empty
             g.k_per_split = (int)(each * kScaleBlock);
         }

@@ -1,0 +1,19 @@
+"""What the expert-layer operators allocate and launch, read from the host code on a machine without a GPU (fake_experts.py)."""
+import pytest
+
+from fake_experts import ask
+
+
+@pytest.mark.parametrize("spec", ["tile,bm=16,bn=64,sk=2", "tile,bm=64,bn=64,sk=16", "tile,bm=128,bn=128,sk=1", None])
+def test_nothing_is_split_where_there_is_no_k(spec):
+    """Zeros all the same: one launch, no workspace."""
+    for c in (0, 2):
+        (r,) = ask([{"op": "scaled", "M": 40, "N": 100, "K": 0, "c": c, **({"spec": spec} if spec else {})}])
+        assert r["plan"] == 0 and r["run"] == 0 and r["workspace"] == 0 and len(r["launches"]) == 1, r
+        assert spec is None or r["describe"].endswith("sk=1")
+
+
+@pytest.mark.parametrize("k,splits", [(1, 1), (128, 1), (129, 2), (256, 2), (385, 2), (1024, 2)])
+def test_a_split_has_no_empty_range(k, splits):
+    (r,) = ask([{"op": "scaled", "M": 40, "N": 100, "K": k, "spec": "tile,bm=16,bn=64,sk=2"}])
+    assert r["plan"] == 0 and r["launches"] == [["scaled_tile_kernel", 6, splits]] and (r["workspace"] > 0) == (splits > 1)

@@ -1,4 +1,4 @@
-"""The expert-layer operators on inputs off the ordinary: rows that share memory."""
+"""The expert-layer operators on inputs off the ordinary: rows that share memory, no K."""
 import zlib
 
 import pytest
@@ -60,3 +60,16 @@ def test_operands_of_a_product_that_share_memory(name):
     sa, sb = (torch.rand((1, r), generator=g).cuda().expand(3, r) for r in (50, 60))      # one scale for all blocks of a row
     found = hg.scaled_product(a, sa, b, sb, c="f32")
     assert torch.equal(found, hg.scaled_product(own[0], sa.contiguous(), own[1], sb.contiguous(), c="f32")) and found.abs().max() > 0
+
+
+# ---- no K -------------------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("c", ["f16", "f32"])
+@pytest.mark.parametrize("spec", ["tile,bm=16,bn=64,sk=2", "tile,bm=64,bn=64,sk=16", "rows,bm=16,bn=16", "phased,bm=128,bn=128"])
+def test_no_depth_gives_zeros_whatever_the_kernel(spec, c):
+    m, n = 40, 100
+    out = torch.full((m, n), float("nan"), dtype={"f16": torch.float16, "f32": torch.float32}[c], device="cuda")
+    with hg.ScaledPlan(m, n, 0, c=c, spec=spec) as p:
+        p.run(0, 0, 0, 0, out.data_ptr(), torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+    assert (out == 0).all()
