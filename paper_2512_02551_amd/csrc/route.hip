@@ -471,7 +471,7 @@ __global__ __launch_bounds__(1024) void place_kernel(RouteArgs a)
 template <int L> __global__ __launch_bounds__(256) void route_backward_kernel(RouteArgs a)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t t = (int64_t)blockIdx.x * 4 + wave;
+    const int64_t t = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + wave;
     __shared__ float scores[4][64 * L], grads[4][64 * L];
     if (t >= a.tokens) return;
     float x[L], p[L];
@@ -634,7 +634,10 @@ hgemm_status_t hgemm_route_backward(hgemm_route_plan_t plan, const void* logits,
     a.logits = logits; a.experts = (int*)experts; a.dweights = dweights; a.dlogits = dlogits;
     set_wide(a, logits);
     a.wide = a.wide && aligned(dlogits, per_lane(a.E) * size);
-    back_of(a.E)<<<(a.tokens + 3) / 4, 256, 0, (hipStream_t)hip_stream>>>(a);
+    // a launch has fewer than 2^32 threads along x: from 2^26 - 3 tokens on, two rows of workgroups
+    const unsigned workgroups = ((unsigned)a.tokens + 3) / 4, most = 0xffffffffu / 256;
+    const dim3 grid = workgroups <= most ? dim3(workgroups) : dim3((workgroups + 1) / 2, 2);
+    back_of(a.E)<<<grid, 256, 0, (hipStream_t)hip_stream>>>(a);
     return hipGetLastError() == hipSuccess ? HGEMM_OK : HGEMM_ERR_LAUNCH;
 }
 

@@ -17,3 +17,13 @@ def test_nothing_is_split_where_there_is_no_k(spec):
 def test_a_split_has_no_empty_range(k, splits):
     (r,) = ask([{"op": "scaled", "M": 40, "N": 100, "K": k, "spec": "tile,bm=16,bn=64,sk=2"}])
     assert r["plan"] == 0 and r["launches"] == [["scaled_tile_kernel", 6, splits]] and (r["workspace"] > 0) == (splits > 1)
+
+
+@pytest.mark.parametrize("tokens", [1, 4, 5, (1 << 26) - 4, (1 << 26) - 3, (1 << 26) - 1])
+def test_every_launch_of_the_routing_has_fewer_than_2_32_threads_along_x(tokens):
+    (r,) = ask([{"op": "route", "tokens": tokens, "experts": 8, "k": 1}])
+    assert r["plan"] == r["run"] == r["backward"] == 0
+    for name, x, y in r["launches"]:
+        assert x * 1024 < 1 << 32
+    ((name, x, y),) = r["backward_launches"]
+    assert x * 256 < 1 << 32 and y < 1 << 16 and tokens <= 4 * x * y < tokens + 8

@@ -1,4 +1,4 @@
-"""The expert-layer operators on inputs off the ordinary: rows that share memory, no K."""
+"""The expert-layer operators on inputs off the ordinary: rows that share memory, no K, the most tokens."""
 import zlib
 
 import pytest
@@ -73,3 +73,22 @@ def test_no_depth_gives_zeros_whatever_the_kernel(spec, c):
         p.run(0, 0, 0, 0, out.data_ptr(), torch.cuda.current_stream().cuda_stream)
         torch.cuda.synchronize()
     assert (out == 0).all()
+
+
+# ---- as many tokens as there may be -------------------------------------------------------------------------------------------------------
+
+def test_the_gradient_of_the_most_tokens():
+    t, e = (1 << 26) - 1, 4
+    x = torch.randn((t, e), dtype=torch.float16, device="cuda", generator=torch.Generator(device="cuda").manual_seed(5))
+    chosen = (torch.arange(t, dtype=torch.int32, device="cuda") % e)[:, None].contiguous()
+    dw = torch.ones((t, 1), device="cuda")
+    dx = torch.full((t, e), float("nan"), dtype=torch.float16, device="cuda")
+    with hg.RoutePlan(t, e, 1, renormalise=False) as p:
+        p.backward(x.data_ptr(), chosen.data_ptr(), dw.data_ptr(), dx.data_ptr(), torch.cuda.current_stream().cuda_stream)
+        torch.cuda.synchronize()
+    assert not dx.isnan().any()
+    at = torch.tensor([0, 1, 4, (1 << 25) - 1, 1 << 25, (1 << 25) + 1, (1 << 25) + 4, t - 4, t - 3, t - 2, t - 1], device="cuda")
+    p64 = torch.softmax(x[at].double(), 1)
+    one = torch.nn.functional.one_hot(chosen[at, 0].long(), e).double()
+    want = p64 * (one - (p64 * one).sum(1, keepdim=True))
+    assert ((dx[at].double() - want).abs() <= 2.0 ** -11 * want.abs() + 2.0 ** -20).all()      # one rounding, and fp32 on numbers below 1
