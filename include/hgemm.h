@@ -305,7 +305,8 @@ hgemm_status_t hgemm_quantise(const hgemm_quantise_t* desc, const void* X, const
  *   top2 = 0 the keys are the logits themselves, which order the same.
  *   groups > 1: the experts form `groups` equal groups; a group scores its largest key, or the sum of its
  *   two largest (top2 = 1); the `keep` best groups stay.  The k largest keys are chosen, descending; equal keys
- *   and scores go to the lower index.  A logit or key that is -infinity or NaN is never chosen.
+ *   and scores go to the lower index.  A logit or key that is -infinity or NaN is never chosen (a softmax over +infinity
+ *   is NaN throughout).
  *   weights[t][j] = factor * s, or, renormalise = 1, factor * s / (sum of the chosen s + 1e-20).
  *   Slots without an expert hold expert -1 and weight 0.
  * The order of rows (offsets, rows and tokens; all three or none): rows by expert, within an expert by token.

@@ -122,7 +122,8 @@ __device__ __forceinline__ void wave_sync()
 
 __device__ __forceinline__ float sigmoid_of(float x) { return 1.f / (1.f + expf(-x)); }
 
-// Largest finite logit (0 where there is none) and the sum of exponentials, at least 1: what a softmax needs.
+// Largest logit (0 where all are -infinity) and the sum of exponentials: what a softmax needs.  The largest adds 1 to the sum, so a sum below that is the 0 of a row
+// without any, and counts as 1; a NaN, of an infinite logit, stays.
 template <int L> __device__ __forceinline__ void softmax_of(const float (&x)[L], float& top, float& sum)
 {
     top = -__builtin_inff();
@@ -133,7 +134,8 @@ template <int L> __device__ __forceinline__ void softmax_of(const float (&x)[L],
     sum = 0.f;
 #pragma unroll
     for (int i = 0; i < L; ++i) sum += expf(x[i] - top);
-    sum = fmaxf(wave_sum(sum), 1.f);
+    sum = wave_sum(sum);
+    sum = sum < 1.f ? 1.f : sum;
 }
 
 // The running sum over the lanes.

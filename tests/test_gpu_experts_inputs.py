@@ -1,4 +1,4 @@
-"""The expert-layer operators on inputs off the ordinary: rows that share memory, no K, the most tokens."""
+"""The expert-layer operators on inputs off the ordinary: rows that share memory, no K, the most tokens, infinite logits."""
 import zlib
 
 import pytest
@@ -92,3 +92,30 @@ def test_the_gradient_of_the_most_tokens():
     one = torch.nn.functional.one_hot(chosen[at, 0].long(), e).double()
     want = p64 * (one - (p64 * one).sum(1, keepdim=True))
     assert ((dx[at].double() - want).abs() <= 2.0 ** -11 * want.abs() + 2.0 ** -20).all()      # one rounding, and fp32 on numbers below 1
+
+
+# ---- infinite logits ----------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kind", [torch.float16, torch.float32], ids=str)
+@pytest.mark.parametrize("renormalise", [True, False])
+@pytest.mark.parametrize("e", [8, 200])
+def test_a_softmax_over_an_infinite_logit_is_no_number(e, renormalise, kind):
+    """exp(inf - inf) over its sum: no weight of such a token is a number, as in the formula.  The choice goes by the logits and stays."""
+    x = torch.randn((40, e), generator=gen("infinite", e)).to(kind)
+    x[7, 5] = float("inf")
+    weights, chosen = (v.cpu() for v in hg.route(x.cuda(), 3, renormalise=renormalise)[:2])
+    assert torch.equal(chosen, x.float().sort(stable=True, dim=1, descending=True).indices[:, :3].to(torch.int32)) and chosen[7, 0] == 5
+    bad = torch.zeros(40, dtype=torch.bool)
+    bad[7] = True
+    assert torch.equal(weights.isnan(), bad[:, None].expand(40, 3))
+    dx = hg.route_backward(x.cuda(), chosen.cuda(), torch.ones((40, 3), device="cuda"), renormalise=renormalise).cpu()
+    assert torch.equal(dx.isnan(), bad[:, None].expand(40, e))
+
+
+def test_a_sigmoid_of_an_infinite_logit_is_one():
+    x = torch.randn((40, 64), generator=gen("infinite sigmoid"))
+    x[7, 5] = float("inf")
+    weights, chosen = (v.cpu() for v in hg.route(x.cuda(), 3, score="sigmoid", renormalise=False)[:2])
+    assert chosen[7, 0] == 5 and weights[7, 0] == 1 and torch.isfinite(weights).all()
+    dx = hg.route_backward(x.cuda(), chosen.cuda(), torch.ones((40, 3), device="cuda"), "sigmoid", False).cpu()
+    assert torch.isfinite(dx).all() and dx[7, 5] == 0
