@@ -281,6 +281,8 @@ def quantise(x, q: str = "e4m3", scale: str = "f32", block_rows: int = 1, rows: 
     x, ldx = _rows(x, "x")
     m, k = (x.shape[0] if index is None else index.shape[0]), x.shape[1]
     pi = 0 if index is None else _ints(index, "index", m)
+    if index is not None and not x.shape[0]:
+        x, ldx = x.new_zeros((1, k)), k                   # an index into no rows: the library takes no rows for no index
     p = QuantisePlan(m, k, _type_name(x), q, scale, block_rows, x_rows=0 if index is None else x.shape[0], ldx=ldx)
     bytes_, kind = _torch_type(q), _torch_type(scale)
     new = lambda shape, dtype: torch.empty(shape, dtype=dtype, device=x.device)  # noqa: E731
@@ -322,6 +324,8 @@ def scaled_product(a, scale_a, b, scale_b, K: Optional[int] = None, c: str = "f1
     # a scale for each row of a single block of rows reads the same both ways only where N = 1
     if tuple(scale_a.shape) != (_blocks(K), a.shape[0]):
         raise ValueError("scale_a has another shape")
+    if index is not None and not a.shape[0]:              # as in quantise
+        a, scale_a, ldsa = torch.zeros((1, lda), dtype=torch.uint8, device=a.device).view(a.dtype), scale_a.new_zeros((_blocks(K), 1)), 1
     out = torch.empty((groups, M, N) if groups and not by_rows else (M, N), dtype=_torch_type(c), device=a.device)
     with ScaledPlan(M, N, K, _type_name(a), c, _type_name(scale_a), SCALE_BLOCK if by_block else 1, groups, along, a.shape[0] if index is not None else 0, lda, ldb, 0, ldsa, ldsb, spec) as p:
         p.run(a.data_ptr(), scale_a.data_ptr(), b.data_ptr(), scale_b.data_ptr(), out.data_ptr(), _stream(), po, pi)

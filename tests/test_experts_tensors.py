@@ -135,8 +135,9 @@ def test_rows_of_any_distance_reach_the_kernels_of_16_and_32_bits(library, name,
     rows, cols = x.shape
     hg.quantise(x)
     assert same(library.seen["x"], x)
-    hg.quantise(x, index=ints(9))
-    assert same(library.seen["x"], x)
+    if rows:
+        hg.quantise(x, index=ints(9))
+        assert same(library.seen["x"], x)
     hg.route(x, 1)
     assert same(library.seen["logits"], x)
     dx = hg.route_backward(x, ints(rows, 1), device(torch.zeros(rows, 1)))
@@ -216,3 +217,15 @@ def test_tensors_of_another_device_are_refused(library, monkeypatch):
         with pytest.raises(ValueError, match="cuda:1"):
             function(*operands)
     assert library.launches == len(calls)
+
+
+def test_an_index_into_no_rows_gives_rows_of_zeros(library):
+    """The library takes a source without rows for one that is not indexed: it is handed a row of zeros, which every index inside it reads."""
+    hg.quantise(device(torch.ones(0, 48)), index=ints(6))
+    assert library.desc.x_rows == 1 and library.desc.M == 6 and same(library.seen["x"], device(torch.zeros(1, 48)))
+    for k in (48, 300):
+        blocks, width = experts._blocks(k), experts._up16(k)
+        out = hg.scaled_product(device(torch.ones((0, width), dtype=torch.float8_e4m3fn)), device(torch.ones(blocks, 0)), device(torch.ones((2, 5, width), dtype=torch.float8_e4m3fn)),
+                                device(torch.ones(2, 1, blocks)), K=k, offsets=ints(3), index=ints(6))
+        assert out.shape == (6, 5) and library.desc.a_rows == 1 and library.desc.lda % 16 == 0
+        assert (library.seen["a"] == 0).all() and library.seen["a"].shape == (1, k) and (library.seen["scale_a"] == 0).all() and library.seen["scale_a"].shape == (blocks, 1)

@@ -1,4 +1,4 @@
-"""The expert-layer operators on inputs off the ordinary: rows that share memory, no K, the most tokens, infinite logits."""
+"""The expert-layer operators on inputs off the ordinary: rows that share memory, no K, the most tokens, infinite logits, no tokens."""
 import zlib
 
 import pytest
@@ -119,3 +119,30 @@ def test_a_sigmoid_of_an_infinite_logit_is_one():
     assert chosen[7, 0] == 5 and weights[7, 0] == 1 and torch.isfinite(weights).all()
     dx = hg.route_backward(x.cuda(), chosen.cuda(), torch.ones((40, 3), device="cuda"), "sigmoid", False).cpu()
     assert torch.isfinite(dx).all() and dx[7, 5] == 0
+
+
+# ---- no tokens ------------------------------------------------------------------------------------------------------------------------------
+
+def test_an_index_into_no_rows_gives_zeros():
+    index = torch.tensor([-1, 0, 5, -1], dtype=torch.int32, device="cuda")
+    q, s, qt, st = hg.quantise(torch.ones((0, 200), device="cuda"), index=index, transposed=True)
+    assert q.shape == (4, 208) and (q.float() == 0).all() and (qt.float() == 0).all() and torch.equal(s, torch.full_like(s, 2.0 ** -96 / 448)) and torch.equal(st, torch.full_like(st, 2.0 ** -96 / 448))
+    b, sb, _, _ = hg.quantise(torch.randn((2 * 128, 200), device="cuda"), block_rows=128)
+    offsets = torch.tensor([0, 1, 4], dtype=torch.int32, device="cuda")
+    for c in ("f16", "f32"):
+        out = hg.scaled_product(q[:0], s[:, :0], b.view(2, 128, 208), sb.view(2, 1, 2), K=200, c=c, offsets=offsets, index=index)
+        assert out.shape == (4, 128) and (out == 0).all()
+
+
+def test_a_layer_without_tokens():
+    """Rows of padding alone: an empty result, and weight gradients of zeros."""
+    import test_gpu_expert_layer as layers
+
+    e, k, width, hidden = 4, 2, 256, 384
+    g = gen("no tokens")
+    new = lambda *shape: (0.05 * torch.randn(shape, generator=g)).to(torch.bfloat16).cuda()  # noqa: E731
+    layer = layers.example.ExpertLayer(new(e, hidden, width), new(e, width, hidden), k)
+    out = layer.forward(new(0, width), torch.randn((0, e), device="cuda"))
+    dx, dlogits, dup, ddown = layer.backward(new(0, width))
+    assert out.shape == dx.shape == (0, width) and dlogits.shape == (0, e)
+    assert dup.shape == (e, hidden, width) and ddown.shape == (e, width, hidden) and (dup == 0).all() and (ddown == 0).all()
