@@ -203,7 +203,8 @@ class CombinePlan:
 def _type_name(t) -> str:
     import torch
 
-    names = {torch.float16: "f16", torch.bfloat16: "bf16", torch.float32: "f32", torch.float8_e4m3fn: "e4m3", torch.float8_e5m2: "e5m2", torch.uint8: "e8m0"}
+    names = {torch.float16: "f16", torch.bfloat16: "bf16", torch.float32: "f32", torch.float8_e4m3fn: "e4m3", torch.float8_e5m2: "e5m2", torch.uint8: "e8m0",
+             torch.float8_e8m0fnu: "e8m0"}
     if t.dtype not in names:
         raise TypeError(f"no operator takes {t.dtype}")
     return names[t.dtype]
@@ -297,12 +298,12 @@ def quantise(x, q: str = "e4m3", scale: str = "f32", block_rows: int = 1, rows: 
 
 
 def scaled_product(a, scale_a, b, scale_b, K: Optional[int] = None, c: str = "f16", offsets=None, along: str = "rows", index=None, spec: Optional[str] = None):
-    """C = A B^T of 8-bit floats.  a [M][>= K]; scale_a [blocks of K][M]; b [N][>= K] with scale_b [blocks of N][blocks of K] or
+    """C = A B^T of 8-bit floats.  a [M][>= K]; scale_a [blocks of K][M] in float32, or of a byte in uint8 or float8_e8m0fnu; b [N][>= K] with scale_b [blocks of N][blocks of K] or
     [blocks of K][N].  With `offsets` [groups + 1]: along = "rows": b [groups][N][>= K], scale_b [groups][blocks of N][blocks of K], and
     `index` [rows] gathers the rows of a; along = "depth": C is [groups][M][N].  K defaults to the width of a."""
     import torch
 
-    if a.dtype not in (torch.float8_e4m3fn, torch.float8_e5m2) or b.dtype != torch.float8_e4m3fn or scale_a.dtype != scale_b.dtype:
+    if a.dtype not in (torch.float8_e4m3fn, torch.float8_e5m2) or b.dtype != torch.float8_e4m3fn or _type_name(scale_a) != _type_name(scale_b):
         raise TypeError("scaled_product needs a in e4m3 or e5m2, b in e4m3 and scales of one type")
     K = min(a.shape[1], b.shape[-1]) if K is None else K
     if K > a.shape[1] or K > b.shape[-1]:

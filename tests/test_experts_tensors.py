@@ -229,3 +229,17 @@ def test_an_index_into_no_rows_gives_rows_of_zeros(library):
                                 device(torch.ones(2, 1, blocks)), K=k, offsets=ints(3), index=ints(6))
         assert out.shape == (6, 5) and library.desc.a_rows == 1 and library.desc.lda % 16 == 0
         assert (library.seen["a"] == 0).all() and library.seen["a"].shape == (1, k) and (library.seen["scale_a"] == 0).all() and library.seen["scale_a"].shape == (blocks, 1)
+
+
+@pytest.mark.parametrize("mixed", [False, True])
+def test_scales_of_a_byte_may_have_torchs_type_for_them(library, mixed):
+    a, b = (device(torch.ones((r, 256), dtype=torch.float8_e4m3fn)) for r in (6, 5))
+    sa, sb = (torch.randint(120, 130, s, dtype=torch.uint8, generator=torch.Generator().manual_seed(1)) for s in ((2, 6), (2, 5)))
+    hg.scaled_product(a, device(sa.view(torch.float8_e8m0fnu)), b, device(sb if mixed else sb.view(torch.float8_e8m0fnu)))
+    assert library.desc.scale == 1 and same(library.seen["scale_a"], device(sa)) and same(library.seen["scale_b"], device(sb))
+    shared = device(sa[:1].view(torch.float8_e8m0fnu)).expand(2, 6)
+    hg.scaled_product(a, shared, b, device(sb))
+    assert same(library.seen["scale_a"], device(sa[:1].expand(2, 6).contiguous()))
+    for wrong in (torch.ones(2, 6), torch.ones((2, 6), dtype=torch.float16)):
+        with pytest.raises((TypeError, ValueError)):
+            hg.scaled_product(a, device(wrong), b, device(sb))

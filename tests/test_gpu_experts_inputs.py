@@ -1,4 +1,4 @@
-"""The expert-layer operators on inputs off the ordinary: rows that share memory, no K, the most tokens, infinite logits, no tokens."""
+"""The expert-layer operators on inputs off the ordinary: rows that share memory, no K, the most tokens, infinite logits, no tokens, types."""
 import zlib
 
 import pytest
@@ -146,3 +146,16 @@ def test_a_layer_without_tokens():
     dx, dlogits, dup, ddown = layer.backward(new(0, width))
     assert out.shape == dx.shape == (0, width) and dlogits.shape == (0, e)
     assert dup.shape == (e, hidden, width) and ddown.shape == (e, width, hidden) and (dup == 0).all() and (ddown == 0).all()
+
+
+# ---- types ------------------------------------------------------------------------------------------------------------------------------------
+
+def test_scales_of_a_byte_in_torchs_type():
+    g = gen("e8m0")
+    a, sa, _, _ = hg.quantise(torch.randn((50, 300), generator=g).cuda(), scale="e8m0")
+    b, sb, _, _ = hg.quantise(torch.randn((70, 300), generator=g).cuda(), scale="e8m0", block_rows=128)
+    own = torch.float8_e8m0fnu
+    want = hg.scaled_product(a, sa, b, sb, K=300)
+    assert torch.equal(hg.scaled_product(a, sa.view(own), b, sb.view(own), K=300), want) and torch.equal(hg.scaled_product(a, sa.view(own), b, sb, K=300), want)
+    one = sa[:1].view(own)
+    assert torch.equal(hg.scaled_product(a, one.expand(3, 50), b, sb, K=300), hg.scaled_product(a, sa[:1].repeat(3, 1), b, sb, K=300))
