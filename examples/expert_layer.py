@@ -35,11 +35,12 @@ class ExpertLayer:
 
     def __init__(self, up, down, k, score="softmax", bias=None):
         self.k, self.score, self.bias = k, score, bias
-        self.load(up, down)
+        self.up, self.down = quantise_weights(up), quantise_weights(down)
 
     def load(self, up, down):
-        """New weights: their 8-bit forms, both ways round."""
-        self.up, self.down = quantise_weights(up), quantise_weights(down)
+        """New weights: their 8-bit forms, both ways round, in the place of the old ones, where a captured step reads them."""
+        for old, new in zip(self.up + self.down, quantise_weights(up) + quantise_weights(down)):
+            old.copy_(new)
 
     @staticmethod
     def _product(a, scale_a, weights, transposed, **more):

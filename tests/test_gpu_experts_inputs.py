@@ -1,4 +1,4 @@
-"""The expert-layer operators on inputs off the ordinary: rows that share memory, no K, the most tokens, infinite logits, no tokens, types."""
+"""The expert-layer operators on inputs off the ordinary: rows that share memory, no K, the most tokens, infinite logits, no tokens, types; and new weights under a captured step."""
 import zlib
 
 import pytest
@@ -159,3 +159,24 @@ def test_scales_of_a_byte_in_torchs_type():
     assert torch.equal(hg.scaled_product(a, sa.view(own), b, sb.view(own), K=300), want) and torch.equal(hg.scaled_product(a, sa.view(own), b, sb, K=300), want)
     one = sa[:1].view(own)
     assert torch.equal(hg.scaled_product(a, one.expand(3, 50), b, sb, K=300), hg.scaled_product(a, sa[:1].repeat(3, 1), b, sb, K=300))
+
+
+# ---- new weights --------------------------------------------------------------------------------------------------------------------------------
+
+def test_a_captured_step_goes_on_with_the_weights_that_are_loaded():
+    import test_gpu_expert_layer as layers
+
+    t, e, k, width, hidden = 12, 4, 2, 256, 384
+    g = gen("load")
+    weights = lambda: [(0.05 * torch.randn(s, generator=g)).to(torch.bfloat16).cuda() for s in ((e, hidden, width), (e, width, hidden))]  # noqa: E731
+    first, second = weights(), weights()
+    x, logits = torch.randn((t, width), generator=g).to(torch.bfloat16).cuda(), torch.randn((t, e), generator=g).cuda()
+    layer = layers.example.ExpertLayer(*first, k)
+    step = layers.example.DecodeStep(layer, t, e, width, hidden)
+    want = [layers.example.ExpertLayer(*w, k).forward(x, logits) for w in (first, second)]
+    assert not torch.equal(*want)
+    for i in (0, 1, 0, 1):
+        layer.load(*(first, second)[i])
+        held = [torch.full((e, hidden, width), 255, dtype=torch.uint8, device="cuda") for _ in range(4)]      # on what the old weights gave back, if they did
+        assert torch.equal(step(x, logits), want[i]) and torch.equal(layer.forward(x, logits), want[i]), i
+        del held
