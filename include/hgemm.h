@@ -230,7 +230,7 @@ typedef enum { HGEMM_GROUPS_NONE = 0, HGEMM_GROUPS_ROWS = 1, HGEMM_GROUPS_DEPTH 
  *          Rows of C that no group holds become zero.  With a_rows > 0 row m of the problem is row
  *          index[m] of an A of a_rows rows (its scales likewise); an index outside [0, a_rows) is a row of zeros.
  *   DEPTH  columns offsets[g] .. offsets[g + 1] - 1 of A and B give C[g]; C is groups x M x N.
- *          Offsets are multiples of 128 (other values count rounded down).  An empty group gives zeros.
+ *          Offsets are multiples of 128, or K (other values count rounded down).  An empty group gives zeros.
  * offsets[0] counts as 0, the others are clamped to the problem; they stay on the device, no call waits for them.
  *
  * A and B start on 16 bytes and have leading dimensions that are multiples of 16; of the last 16-byte

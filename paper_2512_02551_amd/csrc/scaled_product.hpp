@@ -98,9 +98,9 @@ __device__ __forceinline__ bool find_tile(const ScaledArgs& a, int mt, int BM, S
     }
     if (a.group == HGEMM_GROUPS_DEPTH) {
         t.g = (int)blockIdx.y;
-        const int lo = t.g == 0 ? 0 : min(max(a.offsets[t.g], 0), a.K) & ~(kScaleBlock - 1);
-        int hi = min(max(a.offsets[t.g + 1], lo), a.K);
-        if (hi != a.K) hi = max(hi & ~(kScaleBlock - 1), lo);
+        auto boundary = [&](int o) { return o >= a.K ? a.K : max(o, 0) & ~(kScaleBlock - 1); };     // K itself may end inside a block
+        int lo = t.g == 0 ? 0 : boundary(a.offsets[t.g]), hi = max(boundary(a.offsets[t.g + 1]), lo);
+        if (lo == hi) lo = hi = 0;                      // an empty range: also one behind such a K, where no block begins
         t.k_begin = __builtin_amdgcn_readfirstlane(lo);
         t.k_end = __builtin_amdgcn_readfirstlane(hi);
     }

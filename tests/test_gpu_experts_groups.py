@@ -140,3 +140,20 @@ def test_ranges_of_k_as_the_library_runs_them(c, scale):
     want, size, a, sa, b, sb, offsets = problem_of_ranges(4096, lengths, m, n, 1, scale)
     got, desc = run_product(a, sa, b, sb, m, n, 4096, c, offsets=offsets, out_shape=(len(lengths), m, n), a="e5m2", scale=scale, b_rows=1, groups=len(lengths), along="depth")
     check(got, want, bound_of(size, want, c, 16), (desc, c))
+
+
+@pytest.mark.parametrize("c", ["f32", "bf16"])
+@pytest.mark.parametrize("spec", [None] + SPECS)
+def test_ranges_behind_a_k_that_ends_inside_a_block_are_empty(spec, c):
+    """An expert without rows behind the last one that has some: zeros, not the last block once more.  Offsets past K count as K."""
+    m, n = 70, 90
+    for k, lengths, past in ((336, (256, 80, 0, 0), 0), (336, (0, 336, 0), 500), (48, (48, 0), 0), (333, (256, 77, 0), 3)):
+        want, size, a, sa, b, sb, offsets = problem_of_ranges(k, lengths, m, n, 1, "f32")
+        offsets = offsets.clone()
+        offsets[-1] += past
+        try:
+            got, desc = run_product(a, sa, b, sb, m, n, k, c, offsets=offsets, out_shape=(len(lengths), m, n), a="e5m2", b_rows=1, groups=len(lengths), along="depth", spec=spec)
+        except hg.HgemmError as error:
+            assert spec and has_no(spec, k, error)
+            continue
+        check(got, want, bound_of(size, want, c, 3), (desc, c, k))
