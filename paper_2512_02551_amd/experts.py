@@ -234,7 +234,9 @@ def _rows(t, what: str, dims: int = 2):
         raise ValueError(f"{what}: {dims} dimensions with contiguous rows are needed")
     if t.shape[-2] > 1 and t.stride(-2) < t.shape[-1]:
         t = t.contiguous()
-    ld = max(t.stride(-2), t.shape[-1], 1)
+    if not t.shape[-1]:
+        return t, 0                                       # no columns: packed, whatever its strides
+    ld = max(t.stride(-2), t.shape[-1])
     if dims == 3 and t.shape[0] > 1 and t.stride(0) != t.shape[1] * ld:
         raise ValueError(f"{what}: packed groups are needed")
     return t, ld

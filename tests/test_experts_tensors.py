@@ -243,3 +243,18 @@ def test_scales_of_a_byte_may_have_torchs_type_for_them(library, mixed):
     for wrong in (torch.ones(2, 6), torch.ones((2, 6), dtype=torch.float16)):
         with pytest.raises((TypeError, ValueError)):
             hg.scaled_product(a, device(wrong), b, device(sb))
+
+
+def test_matrices_without_columns_are_packed(library):
+    """No K, no N: nothing is read, whatever strides torch gives such tensors; products give zeros."""
+    q = lambda *shape: device(torch.ones(shape, dtype=torch.float8_e4m3fn))  # noqa: E731
+    f = lambda *shape: device(torch.ones(shape))  # noqa: E731
+    assert hg.scaled_product(q(4, 0), f(0, 4), q(6, 0), f(1, 0)).shape == (4, 6) and library.desc.lda == library.desc.ldb == 0 and library.desc.ld_scale_b == 0
+    assert hg.scaled_product(q(4, 0), f(0, 4), q(2, 6, 0), f(2, 1, 0), offsets=ints(3)).shape == (4, 6) and library.desc.ldb == 0
+    assert hg.scaled_product(q(4, 0), f(0, 4), q(6, 0), f(0, 6), offsets=ints(3), along="depth").shape == (2, 4, 6) and library.desc.b_block_rows == 1
+    hg.quantise(f(4, 0), transposed=True)
+    assert library.desc.ldx == 0
+    hg.combine(f(6, 0), ints(4, 2))
+    assert library.desc.ldy == 0
+    dy, dw = hg.combine_backward(f(6, 0), ints(4, 2), ints(6), None, f(4, 0))
+    assert library.desc.ldy == library.desc.ldo == 0 and dy.shape == (6, 0) and dw.shape == (4, 2)

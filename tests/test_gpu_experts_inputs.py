@@ -75,6 +75,18 @@ def test_no_depth_gives_zeros_whatever_the_kernel(spec, c):
     assert (out == 0).all()
 
 
+@pytest.mark.parametrize("c", ["f16", "f32"])
+def test_no_depth_gives_zeros_from_tensors(c):
+    q, s, qt, st = hg.quantise(torch.ones((5, 0), device="cuda"), transposed=True)
+    assert q.shape == (5, 0) and s.shape == (0, 5) and qt.shape == (0, 16) and st.shape == (1, 0)
+    new = lambda *shape: torch.empty(shape, device="cuda")  # noqa: E731
+    b = new(6, 0).to(torch.float8_e4m3fn)
+    assert torch.equal(hg.scaled_product(q, s, b, new(1, 0), c=c).float(), torch.zeros((5, 6), device="cuda"))
+    offsets = torch.tensor([0, 2, 4], dtype=torch.int32, device="cuda")
+    assert torch.equal(hg.scaled_product(q, s, torch.stack([b, b]), new(2, 1, 0), c=c, offsets=offsets).float(), torch.zeros((5, 6), device="cuda"))
+    assert torch.equal(hg.scaled_product(q, s, b, new(0, 6), c=c, offsets=0 * offsets, along="depth").float(), torch.zeros((2, 5, 6), device="cuda"))
+
+
 # ---- as many tokens as there may be -------------------------------------------------------------------------------------------------------
 
 def test_the_gradient_of_the_most_tokens():
