@@ -157,3 +157,33 @@ def test_ranges_behind_a_k_that_ends_inside_a_block_are_empty(spec, c):
             assert spec and has_no(spec, k, error)
             continue
         check(got, want, bound_of(size, want, c, 3), (desc, c, k))
+
+
+# ---- sums whose large products cancel -------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("scale", ["f32", "e8m0"])
+@pytest.mark.parametrize("c", TYPES)
+@pytest.mark.parametrize("spec", [None] + SPECS)
+def test_cancelling_products(spec, c, scale):
+    """Within every block of 128 each large product comes with its negative, at places dealt at random, beside small ones that are what is left: a 16-bit C keeps them to
+    2^-10 of the magnitudes, an fp32 C to roundings of fp32."""
+    g = gen("cancel", scale)
+    m, n, k = 70, 150, 384
+
+    def half(rows):
+        big = torch.exp2(torch.randint(-6, 9, (rows, k // 128, 48), generator=g).float()) * torch.where(torch.rand((rows, k // 128, 48), generator=g) < 0.5, -1.75, 1.0)
+        return big, torch.exp2(torch.randint(-6, 1, (rows, k // 128, 32), generator=g).float())
+
+    (a, small_a), (b, small_b) = half(m), half(n)
+    order = torch.stack([torch.randperm(128, generator=g) for _ in range(k // 128)])
+    a, b = (torch.cat(parts, 2).gather(2, order.expand(len(parts[0]), -1, -1)).flatten(1).to(torch.float8_e4m3fn) for parts in ((a, -a, small_a), (b, b, small_b)))
+    sa, sb = scales(g, (blocks(k), m), scale, 10), scales(g, (blocks(n), blocks(k)), scale)
+    va, vb = ref.by_rows(a, sa, k), ref.by_blocks(b, sb, k)
+    want, size = va @ vb.t(), va.abs() @ vb.abs().t()
+    assert (want.abs() < 0.05 * size).all()
+    try:
+        got, desc = run_product(a, sa, b, sb, m, n, k, c, scale=scale, spec=spec)
+    except hg.HgemmError as error:
+        assert spec and has_no(spec, k, error)
+        return
+    check(got, want, bound_of(size, want, c, blocks(k)), (desc, c))
