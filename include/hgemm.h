@@ -23,7 +23,10 @@
  * stream-K and padded plans own a workspace.
  * The library never prints, never throws, never synchronises the device, and
  * launches only on the stream it is given (Section 2.4.1 forbids a kernel
- * under test from using extra streams).
+ * under test from using extra streams).  A plan whose workspace holds
+ * counters (a split of K joined in one launch, the routing of up to 128
+ * tokens) clears them in the null stream when it is made; its first run waits
+ * for that stream unless it goes there itself.
  */
 #ifndef HGEMM_H
 #define HGEMM_H

@@ -9,6 +9,7 @@ namespace hgemm {
 
 bool current_device_is_gfx950();        // of the calling thread's current device
 int64_t compute_units();
+bool wait_for_clearing(bool& clearing, hipStream_t stream);      // before a run: false if the counters of the plan could not be waited for
 
 constexpr int kScaleBlock = HGEMM_SCALE_BLOCK;
 typedef float f4 __attribute__((ext_vector_type(4)));

@@ -559,6 +559,7 @@ hgemm_status_t check(const hgemm_route_t* d)
 struct hgemm_route_plan_s {
     RouteArgs args;
     void* workspace = nullptr;
+    bool clearing = false;      // the counter of few tokens may still be on its way to zero
 };
 
 extern "C" {
@@ -596,6 +597,7 @@ hgemm_status_t hgemm_route_plan(hgemm_route_plan_t* out, const hgemm_route_t* d)
     }
     (few ? (void*&)a.arrived : (void*&)a.counts) = workspace;
     p->workspace = workspace;
+    p->clearing = few;
     p->args = a;
     *out = p;
     return HGEMM_OK;
@@ -614,6 +616,7 @@ hgemm_status_t hgemm_route_run(hgemm_route_plan_t plan, const void* logits, cons
     a.logits = logits; a.bias = bias; a.weights = weights; a.experts = experts;
     a.offsets = offsets; a.rows = rows; a.tokens_of = tokens_of;
     const hipStream_t s = (hipStream_t)hip_stream;
+    if (!wait_for_clearing(plan->clearing, s)) return HGEMM_ERR_LAUNCH;
     set_wide(a, logits);
     const unsigned blocks = a.blocks ? a.blocks : 1;    // without tokens: padding only
     if (a.tokens <= kPlaceTokens) {

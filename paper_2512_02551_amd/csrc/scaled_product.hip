@@ -164,6 +164,7 @@ struct hgemm_scaled_plan_s {
     int64_t grid_x = 0, grid_y = 1;
     void* workspace = nullptr;
     size_t workspace_bytes = 0;
+    bool clearing = false;      // the counters may still be on their way to zero
 };
 
 namespace {
@@ -267,6 +268,7 @@ hgemm_status_t make_plan_unguarded(hgemm_scaled_plan_t* out, int64_t M, int64_t 
                 return HGEMM_ERR_ALLOC;
             }
             g.counters = (int*)p->workspace;
+            p->clearing = true;
             g.partial = (float*)((char*)p->workspace + counters);
         }
     }
@@ -317,6 +319,7 @@ hgemm_status_t hgemm_scaled_run(hgemm_scaled_plan_t plan, const void* A, const v
     a.index = index;
     const dim3 grid((unsigned)plan->grid_x, (unsigned)plan->grid_y);
     const hipStream_t stream = (hipStream_t)hip_stream;
+    if (!wait_for_clearing(plan->clearing, stream)) return HGEMM_ERR_LAUNCH;
     const ScaledEntry& e = *plan->choice.entry;
     plan->kernel<<<grid, e.threads, e.lds_bytes, stream>>>(a);
     return hipGetLastError() == hipSuccess ? HGEMM_OK : HGEMM_ERR_LAUNCH;

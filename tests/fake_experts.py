@@ -2,7 +2,8 @@
 what their calls launch, on a machine without a GPU.
 
     ask([{"op": "scaled", "M": 8, "N": 8, "K": 8, ...}, {"op": "route", "tokens": 4, ...}, ...]) -> one dict per question: status of the plan, description,
-    workspace bytes, launches as [kernel, grid x, grid y] of one run (and of a gradient).  Operands lie at an address that nothing reads."""
+    workspace bytes, launches as [kernel, grid x, grid y] of one run (and of a gradient) on a stream of its own, and how many of them did not wait for the clearing
+    of the plan's memory.  Operands lie at an address that nothing reads."""
 import ctypes
 import json
 import os
@@ -14,7 +15,7 @@ import tempfile
 HERE = os.path.dirname(os.path.abspath(__file__))
 sys.path.insert(0, os.path.dirname(HERE))
 LIB = os.path.join(os.path.dirname(HERE), "paper_2512_02551_amd", "libhgemm.so")
-BASE = 1 << 36
+BASE, STREAM = 1 << 36, 1 << 20         # STREAM: not the null stream
 
 
 def ask(questions):
@@ -44,7 +45,9 @@ def _scaled(fake, lib, experts, q):
         assert lib.hgemm_scaled_describe(plan, text, 256) == 0
         fake.fake_take_log()
         r["describe"], r["workspace"] = text.value.decode(), lib.hgemm_scaled_workspace_bytes(plan)
-        r["run"], r["launches"] = lib.hgemm_scaled_run(plan, *[BASE] * 5, BASE, BASE, None), _launches(fake)
+        fake.fake_take_overtaken()
+        r["run"], r["launches"] = lib.hgemm_scaled_run(plan, *[BASE] * 5, BASE, BASE, STREAM), _launches(fake)
+        r["overtaken"] = fake.fake_take_overtaken()
         lib.hgemm_scaled_destroy(plan)
     return r
 
@@ -55,9 +58,25 @@ def _route(fake, lib, experts, q):
     r = {"plan": lib.hgemm_route_plan(ctypes.byref(plan), ctypes.byref(d))}
     if r["plan"] == 0:
         fake.fake_take_log()
-        r["run"], r["launches"] = lib.hgemm_route_run(plan, BASE, None, *[BASE] * 5, None), _launches(fake)
-        r["backward"], r["backward_launches"] = lib.hgemm_route_backward(plan, *[BASE] * 4, None), _launches(fake)
+        fake.fake_take_overtaken()
+        r["run"], r["launches"] = lib.hgemm_route_run(plan, BASE, None, *[BASE] * 5, STREAM), _launches(fake)
+        r["overtaken"] = fake.fake_take_overtaken()
+        r["backward"], r["backward_launches"] = lib.hgemm_route_backward(plan, *[BASE] * 4, STREAM), _launches(fake)
         lib.hgemm_route_destroy(plan)
+    return r
+
+
+def _plan(fake, lib, experts, q):
+    """A product of 16-bit floats (hgemm_plan_override)."""
+    plan = ctypes.c_void_p()
+    i64 = ctypes.c_int64
+    r = {"plan": lib.hgemm_plan_override(ctypes.byref(plan), i64(q["M"]), i64(q["N"]), i64(q["K"]), None, q["spec"].encode())}
+    if r["plan"] == 0:
+        r["workspace"] = lib.hgemm_plan_workspace_bytes(plan)
+        fake.fake_take_overtaken()
+        r["run"] = lib.hgemm_run(plan, *[ctypes.c_void_p(BASE)] * 3, ctypes.c_void_p(STREAM))
+        r["overtaken"] = fake.fake_take_overtaken()
+        lib.hgemm_destroy(plan)
     return r
 
 
@@ -68,6 +87,7 @@ if __name__ == "__main__":
     from paper_2512_02551_amd import experts as experts_module
     hgemm_lib = ctypes.CDLL(LIB)
     experts_module.declare(hgemm_lib)
-    answers = [{"scaled": _scaled, "route": _route}[q["op"]](fake_lib, hgemm_lib, experts_module, q) for q in json.load(sys.stdin)]
+    hgemm_lib.hgemm_plan_workspace_bytes.restype = ctypes.c_size_t
+    answers = [{"scaled": _scaled, "route": _route, "plan": _plan}[q["op"]](fake_lib, hgemm_lib, experts_module, q) for q in json.load(sys.stdin)]
     assert fake_lib.fake_live_bytes() == 0, "a plan's memory was not given back"
     print(json.dumps(answers))

@@ -19,11 +19,20 @@ uintptr_t g_next = (uintptr_t)1 << 40;
 dim3 g_grid, g_block;
 size_t g_shared = 0;
 hipStream_t g_stream = nullptr;
+bool g_clearing = false;        // a hipMemset is on its way in the null stream: it returns before it has run
+int g_overtaken = 0;
 }  // namespace
 
 extern "C" {
 void fake_device_memory(size_t bytes) { g_limit = bytes; }
 size_t fake_live_bytes() { return g_live_bytes; }
+// Launches since the last time that went to another stream than the null stream while a hipMemset could still have been on its way.
+int fake_take_overtaken()
+{
+    const int n = g_overtaken;
+    g_overtaken = 0;
+    return n;
+}
 // What was called since the last time, one line each: "malloc BYTES", "malloc BYTES failed", "free", "launch KERNEL GRIDX GRIDY"
 // (the generic kernel: followed by A, B, C, M, N, K, lda, ldb, ldc).
 const char* fake_take_log()
@@ -48,8 +57,9 @@ hipError_t __hipPopCallConfiguration(dim3* grid, dim3* block, size_t* shared, hi
     *grid = g_grid; *block = g_block; *shared = g_shared; *stream = g_stream;
     return hipSuccess;
 }
-hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3, void** args, size_t, hipStream_t)
+hipError_t hipLaunchKernel(const void* f, dim3 grid, dim3, void** args, size_t, hipStream_t stream)
 {
+    g_overtaken += g_clearing && stream;
     g_log += "launch " + g_names[f] + " " + std::to_string(grid.x) + " " + std::to_string(grid.y);
     if (g_names[f].find("generic_gemm_kernel") != std::string::npos)      // (A, B, C, M, N, K, lda, ldb, ldc, col_major): three pointers, six int64
         for (int i = 0; i < 9; ++i) g_log += " " + std::to_string(*(const int64_t*)args[i]);
@@ -67,7 +77,16 @@ hipError_t hipGetDevicePropertiesR0600(hipDeviceProp_tR0600* p, int)
 hipError_t hipGetLastError() { return hipSuccess; }
 hipError_t hipFuncSetAttribute(const void*, hipFuncAttribute, int) { return hipSuccess; }
 hipError_t hipGetSymbolAddress(void** p, const void*) { *p = (void*)((uintptr_t)1 << 39); return hipSuccess; }
-hipError_t hipMemset(void*, int, size_t) { return hipSuccess; }
+hipError_t hipMemset(void*, int, size_t)
+{
+    g_clearing = true;
+    return hipSuccess;
+}
+hipError_t hipStreamSynchronize(hipStream_t stream)
+{
+    if (!stream) g_clearing = false;
+    return hipSuccess;
+}
 hipError_t hipMalloc(void** p, size_t bytes)
 {
     const bool ok = bytes <= g_limit && g_live_bytes <= g_limit - bytes;

@@ -27,3 +27,13 @@ def test_every_launch_of_the_routing_has_fewer_than_2_32_threads_along_x(tokens)
         assert x * 1024 < 1 << 32
     ((name, x, y),) = r["backward_launches"]
     assert x * 256 < 1 << 32 and y < 1 << 16 and tokens <= 4 * x * y < tokens + 8
+
+
+@pytest.mark.parametrize("question", [
+    {"op": "scaled", "M": 64, "N": 512, "K": 8192, "spec": "tile,bm=64,bn=64,sk=8"}, {"op": "route", "tokens": 32, "experts": 64, "k": 4}, {"op": "route", "tokens": 500, "experts": 64, "k": 4},
+    {"op": "plan", "M": 64, "N": 512, "K": 8192, "spec": "skinny,sk=8,fr=1"},
+], ids=lambda q: "-".join(map(str, q.values())))
+def test_a_run_finds_the_counters_of_a_new_plan_cleared(question):
+    """They are cleared in the null stream, which other streams do not wait for, and a clearing returns before it has run."""
+    (r,) = ask([question])
+    assert r["plan"] == r["run"] == 0 and r.get("workspace", 1) > 0 and r["overtaken"] == 0

@@ -1,4 +1,4 @@
-"""The expert-layer operators on inputs off the ordinary: rows that share memory, no K, the most tokens, infinite logits, no tokens, types; and new weights under a captured step."""
+"""The expert-layer operators on inputs off the ordinary: rows that share memory, no K, the most tokens, infinite logits, no tokens, types, new weights under a captured step, new plans beside a busy stream."""
 import zlib
 
 import pytest
@@ -192,3 +192,32 @@ def test_a_captured_step_goes_on_with_the_weights_that_are_loaded():
         held = [torch.full((e, hidden, width), 255, dtype=torch.uint8, device="cuda") for _ in range(4)]      # on what the old weights gave back, if they did
         assert torch.equal(step(x, logits), want[i]) and torch.equal(layer.forward(x, logits), want[i]), i
         del held
+
+
+# ---- streams ------------------------------------------------------------------------------------------------------------------------------------
+
+def test_a_new_plan_runs_on_a_stream_beside_a_busy_null_stream():
+    """Its counters are cleared in the null stream; the other stream does not wait for that, so the plan has to."""
+    g = gen("busy")
+    m, n, k, t, e = 64, 512, 8192, 32, 64
+    a, sa, _, _ = hg.quantise(torch.randn((m, k), generator=g).cuda())
+    b, sb, _, _ = hg.quantise(torch.randn((n, k), generator=g).cuda(), block_rows=128)
+    x, w = torch.randn((m, k), generator=g).half().cuda(), torch.randn((k, n), generator=g).half().cuda()
+    logits = torch.randn((t, e), generator=g).cuda()
+    new = lambda *shape, dtype=torch.int32: torch.full(shape, -7, dtype=dtype, device="cuda")  # noqa: E731
+    want = hg.scaled_product(a, sa, b, sb, spec="tile,bm=64,bn=64,sk=8"), hg.hgemm(x, w, spec="skinny,sk=8,fr=1"), *hg.route(logits, 4)
+    big, side = torch.randn((8192, 8192), device="cuda").half(), torch.cuda.Stream()
+    c, d = torch.zeros_like(want[0]), torch.zeros_like(want[1])
+    order = torch.zeros_like(want[2]), new(t, 4), new(e + 1), new(t, 4), new(t * 4)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        big @ big                                                 # some milliseconds ahead of the clearing
+    with hg.ScaledPlan(m, n, k, spec="tile,bm=64,bn=64,sk=8") as p, hg.Plan(m, n, k, spec="skinny,sk=8,fr=1") as q, hg.RoutePlan(t, e, 4, "f32") as r:
+        assert p.workspace_bytes() > 0 and q.workspace_bytes() > 0
+        s = side.cuda_stream
+        p.run(a.data_ptr(), sa.data_ptr(), b.data_ptr(), sb.data_ptr(), c.data_ptr(), s)
+        q.run(x.data_ptr(), w.data_ptr(), d.data_ptr(), s)
+        r.run(logits.data_ptr(), 0, *[o.data_ptr() for o in order], s)
+        torch.cuda.synchronize()
+    for got, expected in zip((c, d, *order), want):
+        assert torch.equal(got, expected)
