@@ -217,10 +217,11 @@ typedef enum { HGEMM_GROUPS_NONE = 0, HGEMM_GROUPS_ROWS = 1, HGEMM_GROUPS_DEPTH 
  *   C[m][n] = sum over blocks b of K of  sa(m, b) * sb(n, b) * sum over k in b of A[m][k] * B[n][k].
  * A is M x K and B is N x K, both K-contiguous; C is M x N.  The sum over a block is taken by the
  * matrix cores, scaled, and added to an fp32 sum in the order of the blocks; one rounding to the type of
- * C.  For a 16-bit C the 8-bit instructions take the sums (which drop what lies more than 13 bits below
- * the largest of eight products: 1.6e-5 of the result over normal values); for an fp32 C the fp16 ones do, on
- * bytes widened to fp16, in fp32 throughout.  Scales of A are by row.  Scales of B are by 128 x 128 block (a weight) or by row
- * (the right operand of a weight gradient).
+ * C.  For a 16-bit C the 8-bit instructions take the sums, which drop what lies more than 13 bits below
+ * the largest of eight products: 1.6e-5 of the result over normal values, and at most 2^-10 of the sum of
+ * the products' magnitudes, which shows where large products cancel.  For an fp32 C the fp16 instructions do, on
+ * bytes widened to fp16, in fp32 throughout: a caller that needs such sums asks for an fp32 C.  Scales of A are
+ * by row.  Scales of B are by 128 x 128 block (a weight) or by row (the right operand of a weight gradient).
  *
  *   forward        Y  = X * W^T             A = X by rows,     B = W by blocks
  *   data gradient  dX = dY * W              A = dY by rows,    B = the transposed form of W, by blocks
@@ -320,6 +321,7 @@ hgemm_status_t hgemm_quantise(const hgemm_quantise_t* desc, const void* X, const
  * hgemm_route_backward: dlogits from dweights, given the logits and the choice (through the weights only: the
  * choice itself has no gradient); in the type of the logits.
  * A plan has a workspace and runs on one stream at a time.  Fewer than 2^26 tokens, at most 2^30 choices.
+ * The time of the order grows with the square of the tokens from some 100000 on.
  */
 typedef struct {
     int64_t tokens;

@@ -1,8 +1,9 @@
 // The weighted sum of the experts' rows of a token, and its gradient.
 //
-// Bound by memory: forward every row of Y passes once; backward it passes once for the weights' gradient, beside one pass over dout, and every row of dY
-// goes out once, the padding among them cleared by workgroups of their own.  No atomics: a token's waves hold all that its gradients need.
-// 8191 tokens of 4 rows of 4096 in bf16: 61 us forward (335 MB, 5.5 TB/s), 119 back (608 MB, 5.1 TB/s); a large copy reaches 4.7.
+// Bound by memory: forward every row of Y passes once; backward it passes once for the weights' gradient, beside a pass over dout for every four rows (from memory
+// one, the others from the cache), and every row of dY goes out once, the padding among them cleared by workgroups of their own.  No atomics: a token's
+// waves hold all that its gradients need.  8191 tokens of 4 rows of 4096 in bf16: 61 us forward (335 MB, 5.5 TB/s), 119 back (608 MB, 5.1 TB/s);
+// 4095 of 8 rows 56 and 109 (5.2 TB/s back); a large copy reaches 4.7.
 #include "experts_common.hpp"
 
 using namespace hgemm;
@@ -65,7 +66,7 @@ template <class Y, class O> __global__ __launch_bounds__(256) void combine_kerne
     o.store((O*)a.out + t * a.ldo + n, a.N - n, a.wide);
 }
 
-// WPT waves take a token, all columns of it: dout passes once, beside the token's rows of Y and dY.  The workgroups behind those of the tokens
+// WPT waves take a token, all columns of it: dout passes once for every four of the token's rows of Y and dY.  The workgroups behind those of the tokens
 // look through 64 rows of dY each and clear the padding among them.
 template <class Y, class O, int WPT> __global__ __launch_bounds__(256) void combine_backward_kernel(CombineArgs a)
 {

@@ -10,7 +10,8 @@
 // within the workgroup is a population count, and its place is its expert's first row, plus the choices of earlier workgroups, plus that rank.
 // Up to 128 tokens are chosen for by workgroups of four (32 tokens of 256 experts on one compute unit: 13 us, its issue slots are the bound), and the one
 // that arrives last orders them all.  For more, a second launch takes 128 tokens a workgroup, each of which sums the counts of all (500 x 128 counts
-// of 16000 tokens are 64 KB of cache, and a launch in between costs more).  No result depends on the order of atomics.
+// of 16000 tokens are 64 KB of cache, and a launch in between costs more).  That grows with the square of the tokens and is felt from some 100000 on: 65536 tokens
+// of 256 experts 112 us, 131072 286, 262144 828.  No result depends on the order of atomics.
 #include <new>
 #include <type_traits>
 

@@ -52,8 +52,9 @@ const ScaledEntry* find_entry(const ScaledArgs& a, hgemm_byte_t a_type, const Ch
 
 // Microseconds of one workgroup for a block of K: alone on its compute unit (its own chain of waits), and its share of a unit that `resident` of
 // them fill.  Measured with f32 scales and a 16-bit C: one tile a unit, K of 2048 and 8192 (alone); 4001 x 14336 x 4096 (full).
-// Of 69 problems drawn at random the pick was within 5 % of the fastest of all kernels on 55 and within 15 % on 61, in the mean 5 % behind it (the
-// furthest, 1.4 .. 1.7: groups padded to 128 rows of which most are empty, and rows off the cache lines, neither of which a plan knows of or weighs).
+// Of 60 problems drawn at random (their timings are among the profiles) the pick was within 5 % of the fastest of all kernels on 38 and within 15 % on 50, in the mean
+// 7 % behind it.  Furthest: 29 rows of A where a long K meets few columns (192 x 6528: 11.8 us streaming, 6.8 with K split in eight), and groups padded to
+// 128 rows of which most are empty (79 x 8 of 60 experts 1.3), where a plan knows the rows there is room for and not those there are.
 struct Speed {
     Family family;
     int bm, bn, resident;

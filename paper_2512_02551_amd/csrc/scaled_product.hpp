@@ -135,9 +135,10 @@ __device__ __forceinline__ void store_c(const ScaledArgs& a, const ScaledTile& t
 
 // A fragment: 16 rows of a block of K, 32 bytes a lane.  The 8-bit instructions line the products of eight k up to the largest of them
 // and keep 13 bits below its leading one (measured: 2^16 + 7 * 2^3 is exact, the seven are lost at 2^2), for all three shapes of them; over normal
-// values the sums are 1.6e-5 off.  That is far below the rounding of a 16-bit C (2.0e-4, 1.7e-3), but not of an fp32 C, for which a caller asks
-// where it adds results up: WIDE kernels turn the bytes into fp16, which is exact for both formats, and sum with the fp16 instructions (2e-7), at
-// half the rate.
+// values the sums are 1.6e-5 off, at most 2^-10 of the products' magnitudes, which is more where large products cancel.  Over normal values that is far below the
+// rounding of a 16-bit C (2.0e-4, 1.7e-3), but not of an fp32 C, for which a caller asks where it adds results up or wants such sums: WIDE kernels turn the
+// bytes into fp16, which is exact for both formats, and sum with the fp16 instructions (6e-8 off, the rounding of C in it).  That is half the rate, and felt
+// at every size: fp32 C against fp16 or bf16, 1 x 4096 x 4096 7.8 us and 7.5, 128 x 4096 x 4096 17 and 12, 11008 x 4096 x 8064 with e8m0 scales 722 and 264.
 template <bool WIDE> struct Fragment;
 template <> struct Fragment<false> { i8 v; };
 template <> struct Fragment<true> { half8 v[4]; };

@@ -2,7 +2,8 @@
 quantising, routing and combining.  Argument marshalling only.
 
 The ``*Plan`` classes take raw device pointers and a stream, as :class:`~paper_2512_02551_amd.Plan` does; the lower-case functions take
-torch tensors on the current device, allocate the results and run on torch's current stream.
+torch tensors on the current device, allocate the results and run on torch's current stream.  A function makes its plan in the call: route, route_backward and a
+scaled_product whose K is split own a workspace and wait for their result before they give it back, so these are not for the capture of a graph; plans are.
 """
 from __future__ import annotations
 
