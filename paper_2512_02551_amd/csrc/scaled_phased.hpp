@@ -16,9 +16,9 @@
 // last instruction that needed its fragments, so no wave has to wait for its LDS reads there; and copies are waited for a whole block
 // (four phases) after they were issued, so what is still in flight at a barrier is a compile-time constant.
 //
-// Measured back to back on several cards, bf16 C: 4001 x 14336 x 4096, f32 scales 211 .. 222 us (2.1 .. 2.2 PFLOP/s; the matrix cores busy half of the cycles at
-// 1.9 GHz), 11008 x 4096 x 8064, e8m0 scales 264 .. 280 us (2.6 .. 2.8 PFLOP/s); 4001 x 4 rows of 32 experts, 4096 x 4096, 302 .. 314 us (1.7 .. 1.8 PFLOP/s of
-// rows that exist; with e8m0 scales 270).  fp32 C, 128 x 128: 16 experts' 4096 x 2048 over 8192 rows 197 .. 207 us (0.7 PFLOP/s, 2.7 TB/s of stores).
+// Measured back to back on several cards, bf16 C: 4001 x 14336 x 4096, f32 scales 208 .. 222 us (2.1 .. 2.2 PFLOP/s; the matrix cores busy half of the cycles at
+// 1.9 GHz), 11008 x 4096 x 8064, e8m0 scales 264 .. 280 us (2.6 .. 2.8 PFLOP/s); 4001 x 4 rows of 32 experts, 4096 x 4096, 298 .. 314 us (1.7 .. 1.8 PFLOP/s of
+// rows that exist; with e8m0 scales 270).  fp32 C, 128 x 128: 16 experts' 4096 x 2048 over 8192 rows 194 .. 207 us (0.7 PFLOP/s, 2.7 TB/s of stores).
 // What is left with f32 scales: the multiply-adds for the scales, 128 a lane and block, are issued beside the matrix instructions (1.6 us a block, 1.3 in a library product with one scale), and a tile's start and end, 8
 // us, which nothing covers as one workgroup fills the LDS.
 #pragma once

@@ -4,7 +4,7 @@
 // conflicts, and the block's scales.  What bounds it: small tiles wait for memory -- 16 x 64 ones stream the weights of experts with a few
 // rows each, 24 x 4 rows of 32 experts of 4096 x 2048 in 42 us (219 MB of weights that have rows: 5.2 TB/s; four stages leave room for three workgroups a
 // unit, which cover each other's starts: six stages and two 46 us, three and four 43, but 78 for 72 on 8 x 2 of 8 of 14336 x 4096) -- large ones for
-// the LDS and the multiply-adds of the scales, one for each sum and block: 256 x 256 tiles take 257 us of 4001 x 14336 x 4096, phased ones 211 .. 222.  They serve the
+// the LDS and the multiply-adds of the scales, one for each sum and block: 256 x 256 tiles take 257 us of 4001 x 14336 x 4096, phased ones 208 .. 222.  They serve the
 // K and tile shapes that those do not.
 #pragma once
 #include "scaled_product.hpp"
